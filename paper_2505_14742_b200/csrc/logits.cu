@@ -292,10 +292,15 @@ __device__ __forceinline__ float2 warp_run(float mx, float s, float c1) {
 // With z' = z / tau, q = softmax(z'), the listed probabilities p_j, P = sum p_j and the teacher's remaining mass
 // R = max(0, 1 - P) (0 when the list is renormalised), r = the student's mass on the unlisted tokens, c = P + R:
 //   loss = w tau^2 [ sum_j p_j (log p_j - log q_j) + R (log R - log r) ]
-//   dz_v = w tau (c q_v - p_v)      v listed,      w tau q_v (c - R / r)      otherwise
+//   dz_v = w tau (c q_v - p_v)      v listed,      w tau (c q_v - R q_v / r)      otherwise
 // A byte per word of the slice marks the listed elements while the row is on its way; the first pass, which follows the
 // copy group by group, leaves them out of the sum over the unlisted and sets them to -inf, so r is a sum of its own
-// and not a difference of two sums that may cancel.  R is one, by definition: the listed probabilities and their sum are
+// and not a difference of two sums that may cancel.  It keeps a maximum of its own too, mu: with su = the sum of exp(z'_v - mu) over the unlisted
+// and mx, S the maximum and sum over all,
+//   log r = mu - mx + log su - log S,      q_v / r = exp(z'_v - mu) / su,      q_v = exp(z'_v - mu) exp(mu - mx) / S,
+// so one exponential per unlisted token gives both terms, and neither depends on r itself being a float: a student that is sure of the
+// list (mu 88 below mx) or a finite mask on all others makes it less than 2^-126.
+// R is a difference, by definition: the listed probabilities and their sum are
 // taken in 64 bits when the list comes with a log-sum-exp (one exponential per listed token; in 32 bits R would be known to
 // about 1e-6 absolute, and R / r, the whole gradient of the unlisted tokens, only as well as that over r).
 struct DistillSmem {
@@ -303,7 +308,8 @@ struct DistillSmem {
     float2 lists[kLgWarps];            // maximum and sum of the teacher's list
     double mass[kLgWarps];             // sum of the listed probabilities
     float loss[kLgWarps];
-    float part[4];                     // this CTA's maximum, sum of the unlisted, sum of the listed; loss
+    float part[4];                     // this CTA's maximum and sum of the unlisted, of the listed
+    float total;                       // its share of the loss
 };
 struct DistillParams {
     const void* Z;
@@ -444,16 +450,19 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
         const int next = settle(m + stride, nxt);
         DistillRow after;
         fetch(next + stride, after);
-        // the row's base and sums, in every thread
-        Base b;
-        float unl, lst, c = 1.0f, R = 0.0f, logP = 0.0f, mx;
+        // the row's maxima and sums, of the unlisted and of the listed, in every thread
+        float mu, su, ml, sl, c = 1.0f, R = 0.0f, logP = 0.0f;
         bool dead = false;
+        Base bu;
         {
             const float4 u = sm->warps[lane % kLgWarps];
-            mx = slots_max(fmaxf(u.x, u.z));
-            b.set(mx, c1);
-            unl = slots_sum(at_base(u.x, u.y, b, c1));
-            lst = slots_sum(at_base(u.z, u.w, b, c1));
+            mu = slots_max(u.x);
+            ml = slots_max(u.z);
+            bu.set(mu, c1);
+            su = slots_sum(at_base(u.x, u.y, bu, c1));
+            Base bl;
+            bl.set(ml, c1);
+            sl = slots_sum(at_base(u.z, u.w, bl, c1));
             if (p.t_lse) {
                 const double P = slots_sum(sm->mass[lane % kLgWarps]);
                 R = (float)fmax(0.0, 1.0 - P);
@@ -469,22 +478,28 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
             }
         }
         if (csize > 1) {
-            if (tid == 0) { sm->part[0] = mx; sm->part[1] = unl; sm->part[2] = lst; }
+            if (tid == 0) { sm->part[0] = mu; sm->part[1] = su; sm->part[2] = ml; sm->part[3] = sl; }
             cluster_sync();
             const uint32_t a = mapa_shared(smem_u32(&sm->part[0]), lane < csize ? lane : 0);
-            float pm = -INFINITY, pu = 0.0f, pl = 0.0f;
-            if (lane < csize) { pm = ld_cluster_f32(a); pu = ld_cluster_f32(a + 4); pl = ld_cluster_f32(a + 8); }
-            b.set(warp_max(pm), c1);
-            unl = warp_sum(at_base(pm, pu, b, c1));
-            lst = warp_sum(at_base(pm, pl, b, c1));
+            float pm = -INFINITY, ps = 0.0f, qm = -INFINITY, qs = 0.0f;
+            if (lane < csize) { pm = ld_cluster_f32(a); ps = ld_cluster_f32(a + 4); qm = ld_cluster_f32(a + 8); qs = ld_cluster_f32(a + 12); }
+            mu = warp_max(pm);
+            ml = warp_max(qm);
+            bu.set(mu, c1);
+            su = warp_sum(at_base(pm, ps, bu, c1));
+            Base bl;
+            bl.set(ml, c1);
+            sl = warp_sum(at_base(qm, qs, bl, c1));
         }
-        float S = unl + lst;
+        Base b;
+        b.set(fmaxf(mu, ml), c1);
+        const float gap = ex2(bu.to(b, c1));                     // exp(mu - mx); next to the listed, what it flushes is nothing
+        float S = (su == 0.0f ? 0.0f : su * gap) + at_base(ml, sl, b, c1);
         if (S == INFINITY) S = NAN;                              // a logit of +inf
         dead = dead || S == 0.0f;                                // or no logit above -inf: nothing to learn
-        const float f = cur.w * p.tau / S;
+        const float wt = cur.w * p.tau, f = wt / S;
         if (p.dZ) {
-            const float coef = R > 0.0f ? (unl == 0.0f ? 0.0f : f * (c - R * S / unl)) : f * c;
-            const float co1 = coef * b.unfix();
+            const float co1 = (su == 0.0f ? 0.0f : wt * (c * gap / S - R / su)) * bu.unfix();
             const f32x2 co = pack2(co1, co1);
             const int full = s.n / W;
             T* d = dst(m);
@@ -493,7 +508,7 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
                 uint4 a[4];
                 block_load(row, bl, a);
                 float g[4][W];
-                if (!dead) b.exps<T>(a, [&](f32x2 e, int j, int h) { unpack2(mul2(e, co), g[j][2 * h], g[j][2 * h + 1]); });
+                if (!dead) bu.exps<T>(a, [&](f32x2 e, int j, int h) { unpack2(mul2(e, co), g[j][2 * h], g[j][2 * h + 1]); });
                 else
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -517,31 +532,32 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
                 if (next < p.M) block_fetch<T>(row, from, s.n, bl);
             }, [] { cp_async_commit(); });
             __syncthreads();                                     // the listed entries overwrite what the words' owners stored
-            if (mine(cur) && !dead) d[cur.at - s.begin] = Row<T>::one(f * c * ex2(b.log2_of(cur.z, c1)) - cur.w * p.tau * prob);
+            if (mine(cur) && !dead) d[cur.at - s.begin] = Row<T>::one(f * c * ex2(b.log2_of(cur.z, c1)) - wt * prob);
         } else {
             const T* from = src(next);
             in_groups(nb, [&](int bl) { if (next < p.M) block_fetch<T>(row, from, s.n, bl); }, [] { cp_async_commit(); });
         }
-        // the loss: this warp's terms, the rest's in thread 0
-        const float scale = cur.w * p.tau * p.tau;
+        // the loss: this warp's terms, the rest's in thread 0; logarithms times tau, as the logits are (a finite mask over a tau below 1 is
+        // beyond the floats, its term of the loss need not be)
+        const float logS = p.tau * logf(S);
         float part = 0.0f;
         if (warp * 32 < p.k) {
-            if (!dead && mine(cur) && prob > 0.0f) part = scale * prob * (logp - ((cur.z - b.m) * p.inv_tau - logf(S)));
+            if (!dead && mine(cur) && prob > 0.0f) part = wt * prob * (p.tau * logp - ((cur.z - b.m) - logS));
             part = warp_sum(part);
         }
-        if (rank == 0 && tid == 0 && !dead && R > 0.0f) part += scale * R * (logf(R) - logf(unl / S));
+        if (rank == 0 && tid == 0 && !dead && R > 0.0f) part += wt * R * (p.tau * (logf(R) - logf(su)) - ((bu.m - b.m) - logS));
         if (lane == 0) sm->loss[warp] = part;
         if (csize > 1) {
             __syncthreads();
             if (tid == 0) {
                 float l = 0.0f;
                 for (int i = 0; i < kLgWarps; ++i) l += sm->loss[i];
-                sm->part[3] = l;
+                sm->total = l;
             }
             cluster_sync();
             if (rank == 0 && tid == 0) {
                 float l = 0.0f;
-                for (int r = 0; r < csize; ++r) l += ld_cluster_f32(mapa_shared(smem_u32(&sm->part[3]), r));
+                for (int r = 0; r < csize; ++r) l += ld_cluster_f32(mapa_shared(smem_u32(&sm->total), r));
                 p.loss[m] = l;
             }
         }
