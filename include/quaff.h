@@ -377,6 +377,8 @@ quaff_status_t quaff_topk_logits(const void* Z, int z_dtype, int64_t ldz, int M,
  * for a token without a loss); null means 1.
  *   Z [M][V] bf16 or f32 (z_dtype), 16-byte aligned rows;  t_val [M][k] f32, t_idx [M][k] int32, dense;  1 <= k <= 256
  *   t_lse_opt, row_w_opt [M] f32;  loss [M] f32 (out);  dZ_opt [M][V] in Z's type, nullable, may be Z itself (lddz = ldz)
+ * The unlisted mass R of a t_lse carries the latter's rounding: where no unlisted logit is above -inf, an R of at most
+ * 2^-16 + 2^-20 |t_lse| counts as 0 (all that either model can say is listed); a larger one makes the loss +inf.
  * Rows with w = 0 (not read), with an empty list and no t_lse, or with no logit above -inf: loss 0 and gradient 0.  A
  * listed token with p > 0 whose student logit is -inf makes the loss +inf; a NaN or +inf logit makes the row NaN.
  */

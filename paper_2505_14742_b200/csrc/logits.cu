@@ -302,7 +302,9 @@ __device__ __forceinline__ float2 warp_run(float mx, float s, float c1) {
 // list (mu 88 below mx) or a finite mask on all others makes it less than 2^-126.
 // R is a difference, by definition: the listed probabilities and their sum are
 // taken in 64 bits when the list comes with a log-sum-exp (one exponential per listed token; in 32 bits R would be known to
-// about 1e-6 absolute, and R / r, the whole gradient of the unlisted tokens, only as well as that over r).
+// about 1e-6 absolute, and R / r, the whole gradient of the unlisted tokens, only as well as that over r).  The log-sum-exp itself has 32
+// bits and the error of its sums: where everything visible is listed, R is that error or 0, r is 0, and R log(R / r) would be infinite for about
+// every second row.  Up to 2^-16 + 2^-20 |lse| (what quaff_topk_logits is held to) such an R counts as 0.
 struct DistillSmem {
     float4 warps[kLgWarps];            // maximum and sum of each warp: of the unlisted, of the listed
     float2 lists[kLgWarps];            // maximum and sum of the teacher's list
@@ -497,6 +499,8 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
         float S = (su == 0.0f ? 0.0f : su * gap) + at_base(ml, sl, b, c1);
         if (S == INFINITY) S = NAN;                              // a logit of +inf
         dead = dead || S == 0.0f;                                // or no logit above -inf: nothing to learn
+        // No unlisted token is visible to the student, and what the teacher left is within what its log-sum-exp can tell: all is listed
+        if (su == 0.0f && R < 1.0f && R <= fmaf(0x1p-20f, fabsf(cur.lse), 0x1p-16f)) { c -= R; R = 0.0f; }
         const float wt = cur.w * p.tau, f = wt / S;
         if (p.dZ) {
             const float co1 = (su == 0.0f ? 0.0f : wt * (c * gap / S - R / su)) * bu.unfix();

@@ -132,3 +132,48 @@ def test_listed_tokens_at_the_lowest_value_of_the_type():
     idx = np.tile(np.arange(k, dtype=np.int32), (M, 1))
     for tau in (1.0, 0.5, 0.25):
         check(device_rows(z, torch.float32), val, idx, None, tau, np.full(M, 0.5, np.float32))
+
+
+# ---------------------------------------------------------------- nothing visible is left unlisted
+def restricted(M, V, n, seed, spread=3.0):
+    """Rows with n visible tokens each."""
+    g = np.random.default_rng(seed)
+    z = np.full((M, V), -INF)
+    at = np.argsort(g.random((M, V)), axis=1)[:, :n]
+    np.put_along_axis(z, at, g.standard_normal((M, n)) * spread, 1)
+    return z
+
+
+@pytest.mark.parametrize("V,n,k", [(1, 1, 1), (5, 5, 5), (60, 60, 64), (200, 200, 256), (4000, 1, 1), (4000, 20, 20), (4000, 20, 64), (70000, 33, 64)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("tau", [0.3, 1.0, 2.0])
+def test_a_list_of_all_visible_tokens_leaves_no_rest(V, n, k, dtype, tau):
+    """Teacher and student see the same few tokens and all of them are listed: what 1 - sum p has left is the rounding of the
+    teacher's log-sum-exp, which no logit of the student can carry.  Loss and gradient as from the renormalised list, which
+    rounding changes by at most the 2^-16 + 2^-20 |lse| that the rule allows; lse is below 64 here."""
+    M = 64
+    t = device_rows(restricted(M, V, n, V + n, 4.0 * tau), dtype)
+    g = np.random.default_rng(n)
+    z = t.double().cpu().numpy()
+    z = device_rows(np.where(np.isfinite(z), z + g.standard_normal(z.shape) * tau, z), dtype)
+    val, idx, lse = torch.empty((M, k), device="cuda"), torch.empty((M, k), dtype=torch.int32, device="cuda"), torch.empty(M, device="cuda")
+    Q.quaff_topk_logits(t, tau, val, idx, lse)
+    w = np.ones(M, np.float32)
+    loss, dZ = run(z, val.cpu().numpy(), idx.cpu().numpy(), lse.cpu().numpy(), tau, w)
+    want, grad = run(z, val.cpu().numpy(), idx.cpu().numpy(), None, tau, w)
+    assert np.isfinite(loss).all() and np.isfinite(dZ).all()
+    step = 2.0 ** -16 + 2.0 ** -20 * 64
+    # p changes by that share of itself, |log p - log q| <= 40
+    assert (np.abs(loss - want) <= 40 * step * tau * tau).all(), (loss, want)
+    assert (np.abs(dZ - grad) <= (step + (2.0 ** -7 if dtype == torch.bfloat16 else 0.0)) * tau).all()
+
+
+def test_a_rest_that_the_student_cannot_carry_is_still_an_infinite_loss():
+    """Beyond the resolution of the log-sum-exp the definition holds: the teacher gives mass to tokens that the student rules out."""
+    M, V, k = 3, 4000, 8
+    z = restricted(M, V, k, 3)
+    idx = np.stack([np.flatnonzero(np.isfinite(r)) for r in z]).astype(np.int32)
+    val = np.zeros((M, k), np.float32)
+    lse = (np.log(k) - np.log([0.999, 0.9, 0.1])).astype(np.float32)
+    loss, dZ = run(device_rows(z, torch.float32), val, idx, lse, 1.0, np.ones(M, np.float32))
+    assert (loss == INF).all() and np.isfinite(dZ).all()
