@@ -380,7 +380,8 @@ quaff_status_t quaff_topk_logits(const void* Z, int z_dtype, int64_t ldz, int M,
  * The unlisted mass R of a t_lse carries the latter's rounding: where no unlisted logit is above -inf, an R of at most
  * 2^-16 + 2^-20 |t_lse| counts as 0 (all that either model can say is listed); a larger one makes the loss +inf.
  * Rows with w = 0 (not read), with an empty list and no t_lse, or with no logit above -inf: loss 0 and gradient 0.  A
- * listed token with p > 0 whose student logit is -inf makes the loss +inf; a NaN or +inf logit makes the row NaN.
+ * listed token with p > 0 whose student logit is -inf makes the loss +inf; a NaN or +inf logit makes the row NaN, and so does a
+ * teacher row that had one: a t_lse of NaN, or a listed value of +inf where t_lse is null or +inf.
  */
 quaff_status_t quaff_distill_topk(const void* Z, int z_dtype, int64_t ldz, int M, int V, const float* t_val,
                                   const int32_t* t_idx, int k, const float* t_lse_opt, float temperature,

@@ -466,9 +466,10 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
             bl.set(ml, c1);
             sl = slots_sum(at_base(u.z, u.w, bl, c1));
             if (p.t_lse) {
-                const double P = slots_sum(sm->mass[lane % kLgWarps]);
-                R = (float)fmax(0.0, 1.0 - P);
-                c = (float)fmax(P, 1.0);
+                // NaN stays NaN, from the list or (an empty list of a teacher row with a NaN) from the log-sum-exp alone
+                const double P = slots_sum(sm->mass[lane % kLgWarps]) + (isnan(cur.lse) ? (double)cur.lse : 0.0);
+                R = P < 1.0 ? (float)(1.0 - P) : (P >= 1.0 ? 0.0f : NAN);
+                c = P < 1.0 ? 1.0f : (float)P;
             } else {
                 const float2 l = sm->lists[lane % kLgWarps];
                 const float tm = slots_max(l.x);
@@ -476,6 +477,7 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
                 tb.set(tm, c1);
                 logP = logf(slots_sum(at_base(l.x, l.y, tb, c1)));
                 dead = tm == -INFINITY;                          // nothing listed
+                if (tm == INFINITY) c = logP = NAN;              // a listed value of +inf: inf / inf
                 if (listed) { logp = (cur.t - tb.m) * p.inv_tau - logP; prob = ex2(logp * kLog2e); }
             }
         }
@@ -546,10 +548,10 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
         const float logS = p.tau * logf(S);
         float part = 0.0f;
         if (warp * 32 < p.k) {
-            if (!dead && mine(cur) && prob > 0.0f) part = wt * prob * (p.tau * logp - ((cur.z - b.m) - logS));
+            if (!dead && mine(cur) && !(prob <= 0.0f)) part = wt * prob * (p.tau * logp - ((cur.z - b.m) - logS));
             part = warp_sum(part);
         }
-        if (rank == 0 && tid == 0 && !dead && R > 0.0f) part += wt * R * (p.tau * (logf(R) - logf(su)) - ((bu.m - b.m) - logS));
+        if (rank == 0 && tid == 0 && !dead && !(R <= 0.0f)) part += wt * R * (p.tau * (logf(R) - logf(su)) - ((bu.m - b.m) - logS));
         if (lane == 0) sm->loss[warp] = part;
         if (csize > 1) {
             __syncthreads();

@@ -177,3 +177,39 @@ def test_a_rest_that_the_student_cannot_carry_is_still_an_infinite_loss():
     lse = (np.log(k) - np.log([0.999, 0.9, 0.1])).astype(np.float32)
     loss, dZ = run(device_rows(z, torch.float32), val, idx, lse, 1.0, np.ones(M, np.float32))
     assert (loss == INF).all() and np.isfinite(dZ).all()
+
+
+# ---------------------------------------------------------------- teacher rows that are not finite
+@pytest.mark.parametrize("V", [900, 70003])
+@pytest.mark.parametrize("bad", [float("nan"), INF])
+def test_a_teacher_row_with_nan_or_inf_makes_the_loss_nan(V, bad):
+    """Through the teacher's own list: quaff_topk_logits makes the row's log-sum-exp NaN or +inf."""
+    M, k = 4, 12
+    g = np.random.default_rng(V)
+    t = device_rows(g.standard_normal((M, V)), torch.float32)
+    z = device_rows(g.standard_normal((M, V)), torch.float32)
+    t[1, 7] = bad
+    t[3] = bad if np.isnan(bad) else t[3]                     # a row of nothing else: an empty list
+    val, idx, lse = torch.empty((M, k), device="cuda"), torch.empty((M, k), dtype=torch.int32, device="cuda"), torch.empty(M, device="cuda")
+    Q.quaff_topk_logits(t, 1.0, val, idx, lse)
+    w = np.ones(M, np.float32)
+    loss, dZ = run(z, val.cpu().numpy(), idx.cpu().numpy(), lse.cpu().numpy(), 1.0, w)
+    rows = [1, 3] if np.isnan(bad) else [1]
+    rest = [m for m in range(M) if m not in rows]
+    assert np.isnan(loss[rows]).all() and np.isnan(dZ[rows]).all()
+    assert np.isfinite(loss[rest]).all() and np.isfinite(dZ[rest]).all()
+    if not np.isnan(bad):                                     # the list renormalised: +inf / +inf
+        loss, dZ = run(z, val.cpu().numpy(), idx.cpu().numpy(), None, 1.0, w)
+        assert np.isnan(loss[1]) and np.isnan(dZ[1]).all()
+        assert np.isfinite(loss[rest]).all() and np.isfinite(dZ[rest]).all()
+
+
+def test_a_nan_log_sum_exp_does_not_reach_rows_that_are_not_trained():
+    M, V, k = 3, 500, 4
+    g = np.random.default_rng(1)
+    z = g.standard_normal((M, V))
+    z[1] = -INF
+    val, idx = g.standard_normal((M, k)).astype(np.float32), np.tile(np.arange(k, dtype=np.int32), (M, 1))
+    lse = np.array([np.nan, np.nan, 3.0], np.float32)
+    loss, dZ = run(device_rows(z, torch.float32), val, idx, lse, 1.0, np.array([0.0, 1.0, 1.0], np.float32))
+    assert loss[0] == 0.0 and loss[1] == 0.0 and not dZ[:2].any() and np.isfinite(loss[2])
