@@ -356,7 +356,7 @@ quaff_status_t quaff_mx4_linear_bwd(int M, int K, int N, const quaff_bf16* dY, i
 /*
  * A teacher's top logits: of every row of Z, the k largest in descending order (equal values: the lower index first), and
  * the log-sum-exp of the whole row at a temperature.  One pass over Z.
- *   Z [M][V] bf16 or f32 (z_dtype), 16-byte aligned rows;  1 <= k <= 256;  0 < temperature < inf
+ *   Z [M][V] bf16 or f32 (z_dtype), 16-byte aligned rows;  1 <= k <= 256;  2^-126 <= temperature < inf
  *   val [M][k] f32, idx [M][k] int32 dense;  lse_opt [M] f32, nullable:  log sum_v exp(Z[m][v] / temperature)
  * Entries of -inf (masked tokens) and NaN are never listed; a row with fewer than k others ends with val = -inf, idx = -1.
  * lse is -inf for a row of nothing but -inf, and NaN for a row that holds a NaN.  V * element size <= 1.5 MB (less 512 bytes).
@@ -375,7 +375,7 @@ quaff_status_t quaff_topk_logits(const void* Z, int z_dtype, int64_t ldz, int M,
  * (log r and q_v / r are taken relative to the largest unlisted logit: r itself may be less than any float)
  * which is d loss[m] / d Z[m][v]: w = row_w_opt[m] is the gradient that arrives at the row's loss (1 / number of tokens, 0
  * for a token without a loss); null means 1.
- *   Z [M][V] bf16 or f32 (z_dtype), 16-byte aligned rows;  t_val [M][k] f32, t_idx [M][k] int32, dense;  1 <= k <= 256
+ *   Z [M][V] bf16 or f32 (z_dtype), 16-byte aligned rows;  t_val [M][k] f32, t_idx [M][k] int32, dense;  1 <= k <= 256;  temperature as above
  *   t_lse_opt, row_w_opt [M] f32;  loss [M] f32 (out);  dZ_opt [M][V] in Z's type, nullable, may be Z itself (lddz = ldz)
  * The unlisted mass R of a t_lse carries the latter's rounding: where no unlisted logit is above -inf, an R of at most
  * 2^-16 + 2^-20 |t_lse| counts as 0 (all that either model can say is listed); a larger one makes the loss +inf.

@@ -956,7 +956,7 @@ extern "C" quaff_status_t quaff_topk_logits(const void* Z, int z_dtype, int64_t 
                                             float* lse_opt, quaff_stream_t stream) {
     QUAFF_RETURN_IF(M < 0 || V <= 0 || k <= 0 || (M > 0 && (!Z || !val || !idx)) || ldz < V, QUAFF_ERR_INVALID_ARG);
     QUAFF_RETURN_IF(z_dtype != QUAFF_BF16 && z_dtype != QUAFF_F32, QUAFF_ERR_INVALID_ARG);
-    QUAFF_RETURN_IF(!(temperature > 0.0f) || isinf(temperature), QUAFF_ERR_INVALID_ARG);
+    QUAFF_RETURN_IF(!(temperature >= FLT_MIN) || isinf(temperature), QUAFF_ERR_INVALID_ARG);      // (1 / temperature and that times log2 e are floats)
     const int esz = z_dtype == QUAFF_F32 ? 4 : 2;
     QUAFF_RETURN_IF(k > kLgMaxK || (int64_t)V * esz > (int64_t)kLgMaxCluster * (kLgSliceMax - 64) || M > (1 << 27), QUAFF_ERR_UNSUPPORTED_SHAPE);
     QUAFF_RETURN_IF(!aligned16(Z) || (ldz * esz) % 16, QUAFF_ERR_ALIGNMENT);
@@ -975,7 +975,7 @@ extern "C" quaff_status_t quaff_distill_topk(const void* Z, int z_dtype, int64_t
     QUAFF_RETURN_IF(M < 0 || V <= 0 || k <= 0 || ldz < V || (dZ_opt && lddz < V), QUAFF_ERR_INVALID_ARG);
     QUAFF_RETURN_IF(M > 0 && (!Z || !t_val || !t_idx || !loss), QUAFF_ERR_INVALID_ARG);
     QUAFF_RETURN_IF(z_dtype != QUAFF_BF16 && z_dtype != QUAFF_F32, QUAFF_ERR_INVALID_ARG);
-    QUAFF_RETURN_IF(!(temperature > 0.0f) || isinf(temperature), QUAFF_ERR_INVALID_ARG);
+    QUAFF_RETURN_IF(!(temperature >= FLT_MIN) || isinf(temperature), QUAFF_ERR_INVALID_ARG);      // (1 / temperature and that times log2 e are floats)
     const int esz = z_dtype == QUAFF_F32 ? 4 : 2;
     QUAFF_RETURN_IF(k > kLgMaxK || (int64_t)V * esz > (int64_t)kLgMaxCluster * (kLgSliceMax - 64) || M > (1 << 27), QUAFF_ERR_UNSUPPORTED_SHAPE);
     QUAFF_RETURN_IF(!aligned16(Z) || (ldz * esz) % 16 || (dZ_opt && (!aligned16(dZ_opt) || (lddz * esz) % 16)), QUAFF_ERR_ALIGNMENT);
