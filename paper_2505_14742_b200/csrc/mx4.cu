@@ -273,11 +273,7 @@ __global__ void __launch_bounds__(kPrepThreads) mx4_prep_kernel(const Mx4PrepPar
             p.T[(int64_t)row * p.r + tid] = (uint16_t)(pack_bf16x2(v, 0.0f) & 0xFFFFu);
         }
         v = __fmul_rn(p.scale, v);
-        for (int i = 0; i < p.parts; ++i) {
-            const uint32_t b = pack_bf16x2(v, 0.0f) & 0xFFFFu;
-            p.Tp[((int64_t)row * p.parts + i) * p.rp + tid] = (uint16_t)b;
-            v = __fsub_rn(v, bf16_bits_to_f32(b));
-        }
+        for (int i = 0; i < p.parts; ++i) p.Tp[((int64_t)row * p.parts + i) * p.rp + tid] = (uint16_t)bf16_part(v);
     }
     __syncwarp();
     cluster_sync();               // the partners' sums stay until they are read

@@ -80,6 +80,17 @@ __device__ __forceinline__ void mx4_unpack8(uint32_t codes, uint32_t (&h)[4]) {
         : "r"(codes));
 }
 
+// f32 -> the sum of bf16 parts, one call per part: what is returned is bf16 bits, v becomes what they leave.  An infinity is its first part
+// and zeros (inf - inf would make the sum NaN); a number beyond the largest bf16 begins with that, not with infinity.
+__device__ __forceinline__ uint32_t bf16_part(float& v) {
+    constexpr uint32_t kMax = 0x7F7F0000u;
+    const uint32_t u = __float_as_uint(v), a = u & 0x7FFFFFFFu;
+    const float x = a > kMax && a < 0x7F800000u ? __uint_as_float(kMax | (u & 0x80000000u)) : v;
+    const uint32_t bits = pack_bf16x2(x, 0.0f) & 0xFFFFu;
+    v = a == 0x7F800000u ? 0.0f : __fsub_rn(v, bf16_bits_to_f32(bits));
+    return bits;
+}
+
 // host side, shared between the translation units (arguments are validated by the entry points)
 quaff_status_t mx4_quantize_launch(const void* X, int x_dtype, int64_t ldx, int M, int K, uint8_t* codes, int64_t ldc, uint8_t* scales,
                                    cudaStream_t st);

@@ -212,9 +212,8 @@ __device__ __forceinline__ void mx4_skinny_body(const SkinnyParams& p, int block
                     uint32_t w[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        w[e] = pack_bf16x2(v[2 * e], v[2 * e + 1]);
-                        v[2 * e] = __fsub_rn(v[2 * e], bf16_lo(w[e]));
-                        v[2 * e + 1] = __fsub_rn(v[2 * e + 1], bf16_hi(w[e]));
+                        const uint32_t lo = bf16_part(v[2 * e]);
+                        w[e] = lo | bf16_part(v[2 * e + 1]) << 16;
                     }
                     *reinterpret_cast<uint4*>(t) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
