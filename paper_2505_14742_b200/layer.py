@@ -123,7 +123,11 @@ class Mx4Linear:
         forward : quaff_mx4_linear_fwd      backward: quaff_mx4_linear_bwd
 
     ``saved`` holds what the last forward leaves for its backward, (X, T); a caller that runs the backward of another batch
-    sets it.  Without ``max_tokens`` rows of training (``train=False``) no gradient buffers are made."""
+    sets it.  With ``train=False`` no gradient buffers are made.
+
+    Y has rows of whole 16-byte words whatever N is, as quaff_distill_topk and ``backward`` take them (N columns of a wider buffer where
+    N is not a multiple of 8, or 4 in f32).  Adapters need N % 8 == 0: a head of V tokens is padded with rows of zeros in W and
+    columns of zeros in B, the loss gets ``Y[:, :V]`` (and may write its gradient there), and ``Y[:, V:]`` is cleared before it goes into ``backward``."""
 
     def __init__(self, Wt: torch.Tensor, A: Optional[torch.Tensor], B: Optional[torch.Tensor], lora_scale: float, max_tokens: int,
                  y_dtype: torch.dtype = torch.bfloat16, keep_G: bool = False, train: bool = True):
@@ -138,7 +142,8 @@ class Mx4Linear:
         self.Wc, self.Ws = Q.mx4_empty(N, K, dev)
         Q.quaff_mx4_quantize(Wt, self.Wc, self.Ws)
         self.T = torch.empty((M, r), dtype=torch.bfloat16, device=dev) if r else None
-        self.Y = torch.empty((M, N), dtype=y_dtype, device=dev)
+        w = 16 // torch.empty((), dtype=y_dtype).element_size()
+        self.Y = torch.empty((M, (N + w - 1) // w * w), dtype=y_dtype, device=dev)[:, :N]
         self.dX = torch.empty((M, pitch), dtype=torch.bfloat16, device=dev)[:, :K] if train else None
         self.dA = torch.zeros((K, r), dtype=torch.float32, device=dev) if r and train else None
         self.dB = torch.zeros((r, N), dtype=torch.float32, device=dev) if r and train else None
