@@ -157,7 +157,8 @@ class Mx4Linear:
 
     def forward(self, X: torch.Tensor) -> torch.Tensor:
         M = X.shape[0]
-        assert M <= self.M and X.shape[1] == self.K
+        if M > self.M or X.shape[1] != self.K:
+            raise ValueError(f"Mx4Linear.forward: at most {self.M} rows of {self.K} columns expected, got {tuple(X.shape)}")
         T, Y = (self.T, self.Y) if M == self.M else (self.T[:M] if self.r else None, self.Y[:M])
         Q.quaff_mx4_linear_fwd(X, self.Wc, self.Ws, self.A, self.B, self.lora_scale, T, Y, self.ws, self.status)
         self.saved = (X, T)
@@ -165,6 +166,10 @@ class Mx4Linear:
 
     def backward(self, dY: torch.Tensor, accumulate: bool = False, need_dX: bool = True):
         M = dY.shape[0]
+        if self.dX is None:
+            raise RuntimeError("Mx4Linear.backward: the layer was made with train=False")
+        if self.saved is None:
+            raise RuntimeError("Mx4Linear.backward: no forward to go back from")
         X, T = self.saved
         dX, G = (self.dX, self.G) if M == self.M else (self.dX[:M], self.G[:M] if self.G is not None else None)
         dX = dX if need_dX else None

@@ -69,3 +69,22 @@ def test_an_odd_vocabulary_is_trained_in_a_head_padded_to_eight():
     assert not dB[:, V:].any() and torch.isfinite(loss).all() and torch.isfinite(dX).all() and torch.isfinite(dA).all()
 
 
+def test_a_backward_that_cannot_be_says_so():
+    from paper_2505_14742_b200.layer import Mx4Linear
+    W = torch.ones((64, 64), dtype=torch.bfloat16, device="cuda")
+    X = torch.ones((4, 64), dtype=torch.bfloat16, device="cuda")
+    A, B = torch.ones((64, 8), dtype=torch.bfloat16, device="cuda"), torch.ones((8, 64), dtype=torch.bfloat16, device="cuda")
+    serve = Mx4Linear(W, A, B, 1.0, 4, train=False)
+    for M in (2, 4):                                           # fewer rows than the layer was made for, and as many
+        dY = serve.forward(X[:M]).clone()
+        with pytest.raises(RuntimeError, match="train"):
+            serve.backward(dY)
+    layer = Mx4Linear(W, A, B, 1.0, 4)
+    with pytest.raises(RuntimeError, match="forward"):
+        layer.backward(torch.ones((4, 64), dtype=torch.bfloat16, device="cuda"))
+    layer.forward(X[:2])
+    with pytest.raises(ValueError):                            # the batch of another forward
+        layer.backward(torch.ones((4, 64), dtype=torch.bfloat16, device="cuda"))
+    for bad in (torch.ones((5, 64), dtype=torch.bfloat16, device="cuda"), torch.ones((4, 32), dtype=torch.bfloat16, device="cuda")):
+        with pytest.raises(ValueError):
+            layer.forward(bad)
