@@ -67,7 +67,7 @@ enum { /* `which` of quaff_workspace_bytes */
     QUAFF_WS_HITS = 5,       /* quaff_outlier_hits (depends on K only) */
     QUAFF_WS_BWD_INT8 = 6,   /* quaff_qlinear_bwd_int8 */
     QUAFF_WS_BWD_LEAN = 7,   /* quaff_qlinear_bwd without a transient bf16 copy of the weight (see there) */
-    QUAFF_WS_MX4_MATMUL = 8, /* quaff_mx4_matmul (nOp and r unused) */
+    QUAFF_WS_MX4_MATMUL = 8, /* quaff_mx4_matmul: 0 for every size */
     QUAFF_WS_MX4_FWD = 9,    /* quaff_mx4_linear_fwd (nOp unused) */
     QUAFF_WS_MX4_BWD = 10    /* quaff_mx4_linear_bwd (nOp unused) */
 };
@@ -320,7 +320,8 @@ quaff_status_t quaff_mx4_dequantize(const uint8_t* codes, int64_t ldc, const uin
 /*
  * Y[m][n] = sum_k Xd[m][k] Wd[n][k], Xd [M][K] and Wd [N][K] the values of two MXFP4 matrices; fp32 accumulation, one
  * rounding to Y's type.  The scales are applied by the tensor cores; no operand is expanded.  Any M >= 0, K, N >= 1.
- *   Y [M][N] bf16 or f32 (y_dtype), ldy >= N (any);  status_opt as in quaff_qlinear_fwd;  ws: QUAFF_WS_MX4_MATMUL bytes
+ *   Y [M][N] bf16 or f32 (y_dtype), ldy >= N (any);  status_opt as in quaff_qlinear_fwd
+ *   ws, ws_bytes: not used (QUAFF_WS_MX4_MATMUL is 0); null and 0 will do
  */
 quaff_status_t quaff_mx4_matmul(int M, int K, int N, const uint8_t* Xc, int64_t ldxc, const uint8_t* Xs,
                                 const uint8_t* Wc, int64_t ldwc, const uint8_t* Ws, void* Y, int y_dtype, int64_t ldy,

@@ -545,7 +545,6 @@ static Mx4FwdWorkspace mx4_fwd_workspace(int M, int K, int r) {
     w.total = off;
     return w;
 }
-size_t mx4_matmul_workspace_bytes(int M, int K, int N) { return 0; }
 size_t mx4_fwd_workspace_bytes(int M, int K, int r) { return M < 0 || K <= 0 || r < 0 ? 0 : mx4_fwd_workspace(M, K, r).total; }
 
 }  // namespace quaff
@@ -575,14 +574,12 @@ extern "C" quaff_status_t quaff_mx4_dequantize(const uint8_t* codes, int64_t ldc
 }
 
 extern "C" quaff_status_t quaff_mx4_matmul(int M, int K, int N, const uint8_t* Xc, int64_t ldxc, const uint8_t* Xs, const uint8_t* Wc, int64_t ldwc,
-                                           const uint8_t* Ws, void* Y, int y_dtype, int64_t ldy, int32_t* status_opt, void* ws, size_t ws_bytes,
+                                           const uint8_t* Ws, void* Y, int y_dtype, int64_t ldy, int32_t* status_opt, void* /*ws*/, size_t /*ws_bytes*/,
                                            quaff_stream_t stream) {
     QUAFF_RETURN_IF(M < 0 || K <= 0 || N <= 0 || (M > 0 && (!Xc || !Xs || !Y)) || !Wc || !Ws || ldy < N, QUAFF_ERR_INVALID_ARG);
     QUAFF_RETURN_IF(ldxc < mx4_row_bytes(K) || ldwc < mx4_row_bytes(K), QUAFF_ERR_INVALID_ARG);
     QUAFF_RETURN_IF(y_dtype != QUAFF_BF16 && y_dtype != QUAFF_F32, QUAFF_ERR_INVALID_ARG);
     QUAFF_RETURN_IF(!aligned16(Xc) || !aligned16(Xs) || !aligned16(Wc) || !aligned16(Ws) || !aligned16(Y) || (ldxc % 16) || (ldwc % 16), QUAFF_ERR_ALIGNMENT);
-    const size_t need = mx4_matmul_workspace_bytes(M, K, N);
-    QUAFF_RETURN_IF(M > 0 && need && (!ws || !aligned16(ws) || ws_bytes < need), QUAFF_ERR_WORKSPACE_TOO_SMALL);
     if (M == 0) return QUAFF_OK;
     Mx4Launch l;
     const Mx4Operands o = {M, K, N, Xc, ldxc, Xs, Wc, ldwc, Ws, nullptr, nullptr, 0, 0, Y, y_dtype, ldy, status_opt};

@@ -138,7 +138,6 @@ struct Mx4FrontParams {
 };
 bool mx4_front_prepare(Mx4FrontParams& p, int M, bool want_db);
 quaff_status_t mx4_front_launch(const Mx4FrontParams& p, cudaStream_t st);
-size_t mx4_matmul_workspace_bytes(int M, int K, int N);
 size_t mx4_fwd_workspace_bytes(int M, int K, int r);
 
 }  // namespace quaff

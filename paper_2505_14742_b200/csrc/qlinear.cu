@@ -753,7 +753,7 @@ extern "C" size_t quaff_workspace_bytes(int which, int M, int K, int N, int nOp,
         case QUAFF_WS_BWD_INT8: return bwd_int8_workspace(M, K, N, nOp, r).total;
         case QUAFF_WS_MX4_FWD: return mx4_fwd_workspace_bytes(M, K, r);
         case QUAFF_WS_MX4_BWD: return mx4_bwd_workspace(M, K, N, r).total;
-        case QUAFF_WS_MX4_MATMUL: return mx4_matmul_workspace_bytes(M, K, N);
+        case QUAFF_WS_MX4_MATMUL: return 0;      // its partial sums stay in shared memory
         case QUAFF_WS_CALIBRATE: return round_up((size_t)max(K, 0) * 4, 256) + 256;   // column maxima / flags, sum, ticket
         case QUAFF_WS_HITS: return 2 * round_up((size_t)max(K, 0) * 4, 256) + 256;    // the same, then this batch's indicator
     }
