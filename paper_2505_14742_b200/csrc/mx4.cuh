@@ -105,7 +105,7 @@ enum { kSkinnyDown = 0, kSkinnyParts = 1, kSkinnyFold = 2, kSkinnyTurned = 3 };
 struct SkinnyParams {
     CUtensorMap map_a, map_b;
     int M, nst, per, ranks;         // output rows; stages of 64 contraction elements, of a rank; slices of the contraction
-    int cols, rp, r, rot;           // accumulator columns (r rounded up to 16, times the parts of G); accumulators
+    int cols, rp, r, rot;           // accumulator columns (r rounded up to 16, times the parts of G); accumulators that TMEM holds (a power of two)
     uint32_t tx_bytes;
     float scale, bf16_scale;
     // T and G: bf16 result (G: optional) and scale x the sum in bf16 parts, [rows][parts rp];  dA, dB: f32 result

@@ -10,8 +10,11 @@
 // such groups take turns (8192 x 11008 49 us, 8192 x 4096 20 us with the operands partly in L2; one group 0.7 us more).
 //
 // A tcgen05.mma loses up to one unit in the last place of its running sum, always towards zero, so the error of a chain of n
-// grows like n.  The MMAs of a tile therefore go round robin to up to sixteen accumulators, added up in fp32 at the end: sixteen
-// times as exact at no cost (8192 tokens, one chain: 9e-6 of the result's norm; sixteen: 6e-7).
+// grows like n.  The MMAs of a tile therefore go round robin to as many accumulators as tensor memory holds (up to sixteen; dA has three
+// parts of G beside one another, which leaves 8, 4 and 2 of them for r = 16, 32 and 64), added up in fp32 at the end.  Where that still makes chains of more than
+// kSkChain, the accumulators are two sets: one is drained into fp32 registers while the other is filled.  dA of 8192 tokens x 11008, error over
+// norm, operands of both signs / all positive: r = 16 6e-7 / 7e-7, r = 64 7e-7 / 9e-7 (in one set 1.1e-6 / 1.6e-6 and 4.6e-6 / 1.0e-5,
+// growing with the tokens; the backward without dX 1 us less of 68 and of 82).
 #pragma once
 
 #include "mx4_gemm.cuh"
@@ -26,8 +29,10 @@ template <int MODE> struct SkinnyCfg {
     static constexpr bool kAMn = MODE >= kSkinnyFold, kBMn = MODE != kSkinnyParts;          // operands whose rows are the contraction
     static_assert(kStages * kStageBytes >= 128 * kCols * 4, "a share takes the stages' place");
 };
+constexpr int kSkChain = 32;               // MMAs that one accumulator adds up at most
 struct SkinnySmem {
-    uint64_t full[8], empty[8], acc_full;
+    uint64_t full[8], empty[8];
+    uint64_t acc_full[2], acc_free[2];     // a set of accumulators is complete; is drained
     uint32_t tmem_base;
     AbortCtl abort;
 };
@@ -52,10 +57,14 @@ __device__ __forceinline__ void mx4_skinny_body(const SkinnyParams& p, int block
     const int rank = p.ranks > 1 ? (int)cluster_ctarank() : 0;
     const int m0 = block / p.ranks * 128;
     const int s0 = rank * p.per, count = max(0, min(p.per, p.nst - s0));
-    const uint32_t full0 = smem_u32(&sm->full[0]), empty0 = smem_u32(&sm->empty[0]), acc_full = smem_u32(&sm->acc_full);
+    const uint32_t full0 = smem_u32(&sm->full[0]), empty0 = smem_u32(&sm->empty[0]);
+    const uint32_t acc_full0 = smem_u32(&sm->acc_full[0]), acc_free0 = smem_u32(&sm->acc_free[0]);
+    // one set of p.rot accumulators for all stages, or sets of half as many for `chunk` stages each
+    const bool one_set = 4 * p.per <= kSkChain * p.rot;
+    const int rot = one_set ? p.rot : p.rot / 2, chunk = one_set ? p.per : kSkChain / 4 * rot;
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) { mbar_init(full0 + 8u * s, 1); mbar_init(empty0 + 8u * s, MODE == kSkinnyDown ? 1 + kSkGroup : 1); }
-        mbar_init(acc_full, 1);
+        for (int h = 0; h < 2; ++h) { mbar_init(acc_full0 + 8u * h, 1); mbar_init(acc_free0 + 8u * h, kSkWarps); }
         sm->abort.flag = 0;
         sm->abort.peer = 0;
         fence_barrier_init();
@@ -93,21 +102,26 @@ __device__ __forceinline__ void mx4_skinny_body(const SkinnyParams& p, int block
             const uint32_t idesc = umma_idesc(kCFmtF32, kFmtBF16, 128, 0) | ((uint32_t)(p.cols >> 3) << 17) | (Cfg::kAMn ? 1u << 15 : 0u) | (Cfg::kBMn ? 1u << 16 : 0u);
             constexpr uint32_t a_lbo = Cfg::kAMn ? (uint32_t)(kAtomBytes >> 4) << 16 : 1u << 16, a_adv = Cfg::kAMn ? 128u : 2u;
             constexpr uint32_t b_lbo = Cfg::kBMn ? (uint32_t)(kAtomBytes >> 4) << 16 : 1u << 16, b_adv = Cfg::kBMn ? 128u : 2u;
-            bool ok = true;
+            int set = 0, at = 0;           // sets filled so far; stages of the present one
             for (int i = 0; i < count; ++i) {
-                const uint32_t s = (uint32_t)(i % kStages);
-                if (!mbar_wait(full0 + 8u * s, (uint32_t)(i / kStages) & 1u, abort_flag)) { ok = false; break; }
+                const uint32_t s = (uint32_t)(i % kStages), half = (uint32_t)set & 1u;
+                if (at == 0 && set >= 2 && !mbar_wait(acc_free0 + 8u * half, (uint32_t)(set / 2 - 1) & 1u, abort_flag)) break;
+                if (!mbar_wait(full0 + 8u * s, (uint32_t)(i / kStages) & 1u, abort_flag)) break;
                 tc_fence_after();
                 const uint32_t s_lo = ((base + s * kStageBytes) & 0x3FFFFu) >> 4;
                 const uint32_t a_lo = s_lo | a_lbo, b_lo = (s_lo + (16384u >> 4)) | b_lbo;
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const int n = 4 * i + k;
-                    umma_f16<1>(tmem + (uint32_t)((n & (p.rot - 1)) * p.cols), make_desc(a_lo + k * a_adv, kDescHi), make_desc(b_lo + k * b_adv, kDescHi), idesc, n >= p.rot);
+                    const int n = 4 * at + k;
+                    umma_f16<1>(tmem + (half * rot + (n & (rot - 1))) * p.cols, make_desc(a_lo + k * a_adv, kDescHi), make_desc(b_lo + k * b_adv, kDescHi), idesc, n >= rot);
                 }
                 umma_commit<1>(empty0 + 8u * s);
+                if (++at == chunk || i == count - 1) {
+                    umma_commit<1>(acc_full0 + 8u * half);
+                    ++set;
+                    at = 0;
+                }
             }
-            if (ok) umma_commit<1>(acc_full);
         }
     } else {
         // (quantization: warps 2..9 take the even stages, 10..17 the odd ones, four of each the first block of a stage, four the
@@ -115,7 +129,39 @@ __device__ __forceinline__ void mx4_skinny_body(const SkinnyParams& p, int block
         const int q = warp & 3, row = q * 32 + lane, quad = (warp - 2) >> 2, half = quad & 1;
         const int m = m0 + row;
         bool ok = true;
+        // this thread's columns of its row: sixteen of every 64
+        float sum[Cfg::kCols / 64][16];
+#pragma unroll
+        for (int c = 0; c < Cfg::kCols / 64; ++c)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[c][j] = 0.0f;
+        int drained = 0;
+        auto drain = [&]() {
+            const uint32_t half = (uint32_t)drained & 1u;
+            if (!mbar_wait(acc_full0 + 8u * half, (uint32_t)(drained / 2) & 1u, abort_flag)) return false;
+            tc_fence_after();
+            const int used = min(rot, 4 * (count - drained * chunk));
+#pragma unroll
+            for (int c = 0; c < Cfg::kCols / 64; ++c) {
+                const int cc = c * 64 + quad * 16;
+                for (int a = 0; a < used && cc < p.cols; ++a) {
+                    uint32_t t[16];
+                    tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + (half * rot + a) * p.cols + cc, t);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) sum[c][j] += __uint_as_float(t[j]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(acc_free0 + 8u * half);
+            ++drained;
+            return true;
+        };
         for (int i = quad >> 1; MODE == kSkinnyDown && i < count; i += 2) {
+            // (a set whose stages are quantized; its MMAs wait for nothing else)
+            while (ok && drained < i / chunk) ok = drain();
+            if (!ok) break;
             const uint32_t s = (uint32_t)(i % kStages);
             if (!mbar_wait(full0 + 8u * s, (uint32_t)(i / kStages) & 1u, abort_flag)) { ok = false; break; }
             const unsigned char* src = stages + (size_t)s * kStageBytes + row * 128;
@@ -134,24 +180,16 @@ __device__ __forceinline__ void mx4_skinny_body(const SkinnyParams& p, int block
             *sc = (uint8_t)byte;                                  // rows and columns beyond the matrix are zeros: byte 0
             if (s0 + i == p.nst - 1 && (p.nst & 1)) sc[2] = 0;    // the other half of the last scale tile
         }
+        while (ok && drained * chunk < count) ok = drain();
         if (MODE == kSkinnyDown) named_bar_sync(1, kSkWarps * 32);      // nobody reads a stage any more
-        if (ok && mbar_wait(acc_full, 0, abort_flag)) {
-            tc_fence_after();
+        if (ok) {
             float* share = reinterpret_cast<float*>(stages) + row * p.cols;
-            const int used = min(p.rot, 4 * count);
-            for (int cc = quad * 16; cc < p.cols; cc += 64) {
-                float sum[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j) sum[j] = 0.0f;
-                for (int a = 0; a < used; ++a) {
-                    uint32_t t[16];
-                    tmem_ld_32x16(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(a * p.cols + cc), t);
-                    tmem_ld_wait();
+            for (int c = 0; c < Cfg::kCols / 64; ++c) {
+                const int cc = c * 64 + quad * 16;
+                if (cc >= p.cols) continue;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) sum[j] += __uint_as_float(t[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(share + cc + j) = make_float4(sum[j], sum[j + 1], sum[j + 2], sum[j + 3]);
+                for (int j = 0; j < 16; j += 4) *reinterpret_cast<float4*>(share + cc + j) = make_float4(sum[c][j], sum[c][j + 1], sum[c][j + 2], sum[c][j + 3]);
             }
         }
     }
