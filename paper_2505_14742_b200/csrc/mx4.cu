@@ -404,7 +404,9 @@ __global__ void __launch_bounds__(kSkThreads, 1) mx4_front_kernel(const __grid_c
 // stages per slice and at most kFrontItems items of the weight per warp; false if not.  Measured, us back to back (on the device), backward
 // of tokens x columns x rows of W, one launch / three on three streams: 515 x 1000 x 1544, r = 8 24.9 / 28.5 (20.2 / 20.1); 1 x 1024 x 1024
 // 27.2 / 36.1 (13.0 / 11.8); 1024 x 2048 x 2048 32.9 / 36.9 (30.4 / 28.5); 3000 x 4096 x 2048 61.2 / 67.8 (57.9 / 64.6); 512 x 2048 x 4096
-// 33.4 / 37.1 (28.3 / 26.6).  Longer slices keep too few CTAs at work: 8192 x 1024 x 1024 (128 stages) 62.0 / 46.3 (58.6 / 41.1).
+// 33.4 / 37.1 (28.3 / 26.6).  Longer slices keep too few CTAs at work: 8192 x 1024 x 1024 (128 stages) 62.0 / 46.3 (58.6 / 41.1).  So the rule is for
+// calls from the host, which it makes 4 to 9 us cheaper; in a captured step it costs up to 2 us.  It does not ask whether the stream is being captured:
+// the slices, and with them the last bits of G and dB, would then differ between a call and its graph.
 constexpr int kFrontItems = 8, kFrontStages = 48;
 bool mx4_front_prepare(Mx4FrontParams& p, int M, bool want_db) {
     const Mx4Device* d = mx4_device();
@@ -609,9 +611,11 @@ extern "C" quaff_status_t quaff_mx4_linear_fwd(int M, int K, int N, const quaff_
     const Mx4Device* d = mx4_device();
     if (!d) return QUAFF_ERR_CUDA;
     // Up to 16 tokens, and row tiles few enough for clusters of four: everything in one launch, each row tile quantizing X and
-    // multiplying it with A for itself.  More row tiles mean longer shares of K per CTA, and A comes from L2 once per tile: then two
-    // launches are better.  One / two launches, us (tokens, K -> N, r): 1, 4096 -> 4096, 16 8.6 / 8.9; 16, 4096 -> 4096, 64 11.0 / 15.2; 1, 1024 -> 1024,
-    // 16 6.2 / 7.0; 1, 11008 -> 4096, 16 13.0 / 12.3; 1, 4096 -> 8192, 16 11.4 / 9.0; 16, 4096 -> 11008, 64 20.7 / 16.7; host time 10.4 / 12.6.
+    // multiplying it with A for itself.  More row tiles mean longer shares of K per CTA, and A comes from L2 once per tile: then two launches
+    // are better.  One / two launches, us on the device with weights that have left L2 (tokens, K -> N, r): 1, 1024 -> 1024, 16 6.0 / 7.0; 1, 11008 -> 1024, 16
+    // 9.7 / 12.5; 16, 11008 -> 1024, 64 12.1 / 22.1; 1, 4096 -> 4096, 16 10.5 / 9.3; 16, 4096 -> 4096, 64 13.8 / 15.9; 1, 8192 -> 4096, 16 13.3 / 12.3; 1, 8192 -> 4096, 64
+    // 14.5 / 16.7; 1, 11008 -> 4096, 16 14.7 / 15.4; 16, 11008 -> 4096, 16 16.7 / 16.3; 16, 11008 -> 4096, 64 18.1 / 24.3.  Where one launch loses on the device
+    // (r = 16, N = 4096, by 1.2 at most, with no order in K) it saves 2 to 3 us of the host's time; warm: 1, 4096 -> 8192, 16 11.4 / 9.0; 16, 4096 -> 11008, 64 20.7 / 16.7.
     if (M <= kMsFusedTokens && ceil_div(N, 128) <= d->clusters[4]) {
         Mx4SmallParams p;
         memset(&p, 0, sizeof(p));

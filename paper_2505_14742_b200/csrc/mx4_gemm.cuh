@@ -68,7 +68,7 @@ struct Mx4Smem {
     uint64_t full[kMxStages], empty[kMxStages];
     uint64_t scales[kMxSfSlots];   // a slot's scales are in TMEM
     uint64_t acc_full;       // a tile's accumulator is complete
-    uint64_t acc_shared;     // its 64 shared columns are drained
+    uint64_t acc_shared;     // its 96 shared columns are drained (with the rest of their half)
     uint64_t acc_empty;      // all of it is drained
     uint32_t tmem_base;
     AbortCtl abort;

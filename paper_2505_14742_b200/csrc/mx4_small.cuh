@@ -15,8 +15,8 @@
 // stage's operand (a thread has one block of 32 columns) while the tensor core multiplies it with A (turned round too: the
 // accumulator rows are ranks of A); every row tile repeats that, which costs A from L2 once more per tile.  The shares of T are added up
 // like those of Y, and s T B is added in fp32, the column of B fetched into registers while the tensor core works.  What it saves is
-// the launch in front: 1 token through 4096 x 4096, r = 16: 8.6 us instead of 8.9, and 10.4 us of host time instead of 12.6; 16 tokens, r = 64:
-// 11.0 instead of 15.2.  The dispatch in mx4.cu has more sizes.
+// the launch in front: through 4096 x 4096 with everything in L2, 1 token, r = 16: 8.6 us instead of 8.9, and 10.4 us of host time instead of 12.6; 16 tokens,
+// r = 64: 11.0 instead of 15.2.  The dispatch in mx4.cu has more sizes, with weights from HBM.
 //
 // Not fused, but behind a kernel that makes codes, scales and s T and lets this one start early (mx4_prep_kernel, mx4_skinny), the
 // producer fetches W ahead of griddepcontrol.wait: W was complete before that kernel passed its own.
