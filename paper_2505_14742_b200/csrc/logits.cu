@@ -295,11 +295,11 @@ __device__ __forceinline__ float2 warp_run(float mx, float s, float c1) {
 //   dz_v = w tau (c q_v - p_v)      v listed,      w tau (c q_v - R q_v / r)      otherwise
 // A byte per word of the slice marks the listed elements while the row is on its way; the first pass, which follows the
 // copy group by group, leaves them out of the sum over the unlisted and sets them to -inf, so r is a sum of its own
-// and not a difference of two sums that may cancel.  It keeps a maximum of its own too, mu: with su = the sum of exp(z'_v - mu) over the unlisted
-// and mx, S the maximum and sum over all,
-//   log r = mu - mx + log su - log S,      q_v / r = exp(z'_v - mu) / su,      q_v = exp(z'_v - mu) exp(mu - mx) / S,
-// so one exponential per unlisted token gives both terms, and neither depends on r itself being a float: a student that is sure of the
-// list (mu 88 below mx) or a finite mask on all others makes it less than 2^-126.
+// and not a difference of two sums that may cancel.  It may be less than 2^-126 (a student that is sure of the list; a finite mask on all others), its
+// logarithm and the shares q_v / r are not.  So the unlisted have a maximum of their own, mu; where it is far below mx, that over all, their exponentials are
+// relative to it: with su = the sum of exp(z'_v - mu) and S the sum of exp(z'_v - mx) over all,
+//   log r = mu - mx + log su - log S,      q_v / r = exp(z'_v - mu) / su,      q_v = exp(z'_v - mu) exp(mu - mx) / S:
+// one exponential per token either way.
 // R is a difference, by definition: the listed probabilities and their sum are
 // taken in 64 bits when the list comes with a log-sum-exp (one exponential per listed token; in 32 bits R would be known to
 // about 1e-6 absolute, and R / r, the whole gradient of the unlisted tokens, only as well as that over r).  The log-sum-exp itself has 32
@@ -310,7 +310,8 @@ struct DistillSmem {
     float2 lists[kLgWarps];            // maximum and sum of the teacher's list
     double mass[kLgWarps];             // sum of the listed probabilities
     float loss[kLgWarps];
-    float part[4];                     // this CTA's maximum and sum of the unlisted, of the listed
+    alignas(16) float part[4];         // this CTA's maximum and sum of the unlisted, of the listed
+    float2 base;                       // what the sums are relative to
     float total;                       // its share of the loss
 };
 struct DistillParams {
@@ -452,19 +453,22 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
         const int next = settle(m + stride, nxt);
         DistillRow after;
         fetch(next + stride, after);
-        // the row's maxima and sums, of the unlisted and of the listed, in every thread
+        // the row's maxima and sums, of the unlisted (relative to `bu`) and of all (to `b`), in every thread
         float mu, su, ml, sl, c = 1.0f, R = 0.0f, logP = 0.0f;
         bool dead = false;
-        Base bu;
+        Base b, bu;
+        auto bases = [&]() {
+            b.set(fmaxf(mu, ml), c1);
+            bu.set(mu, c1);
+            if (bu.to(b, c1) > -60.0f) bu = b;                   // (then r is an ordinary number, and more exact without a factor for the whole row)
+        };
         {
             const float4 u = sm->warps[lane % kLgWarps];
             mu = slots_max(u.x);
             ml = slots_max(u.z);
-            bu.set(mu, c1);
+            bases();
             su = slots_sum(at_base(u.x, u.y, bu, c1));
-            Base bl;
-            bl.set(ml, c1);
-            sl = slots_sum(at_base(u.z, u.w, bl, c1));
+            sl = slots_sum(at_base(u.z, u.w, b, c1));
             if (p.t_lse) {
                 // NaN stays NaN, from the list or (an empty list of a teacher row with a NaN) from the log-sum-exp alone
                 const double P = slots_sum(sm->mass[lane % kLgWarps]) + (isnan(cur.lse) ? (double)cur.lse : 0.0);
@@ -482,23 +486,22 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
             }
         }
         if (csize > 1) {
-            if (tid == 0) { sm->part[0] = mu; sm->part[1] = su; sm->part[2] = ml; sm->part[3] = sl; }
+            if (tid == 0) {
+                *reinterpret_cast<float4*>(sm->part) = make_float4(mu, su, ml, sl);
+                sm->base = make_float2(bu.m, b.m);
+            }
             cluster_sync();
-            const uint32_t a = mapa_shared(smem_u32(&sm->part[0]), lane < csize ? lane : 0);
-            float pm = -INFINITY, ps = 0.0f, qm = -INFINITY, qs = 0.0f;
-            if (lane < csize) { pm = ld_cluster_f32(a); ps = ld_cluster_f32(a + 4); qm = ld_cluster_f32(a + 8); qs = ld_cluster_f32(a + 12); }
-            mu = warp_max(pm);
-            ml = warp_max(qm);
-            bu.set(mu, c1);
-            su = warp_sum(at_base(pm, ps, bu, c1));
-            Base bl;
-            bl.set(ml, c1);
-            sl = warp_sum(at_base(qm, qs, bl, c1));
+            const uint32_t a = mapa_shared(smem_u32(&sm->part[0]), lane < csize ? lane : 0), ab = mapa_shared(smem_u32(&sm->base), lane < csize ? lane : 0);
+            float4 u = make_float4(-INFINITY, 0.0f, -INFINITY, 0.0f);
+            if (lane < csize) u = ld_cluster_f4(a);
+            mu = warp_max(u.x);
+            ml = warp_max(u.z);
+            bases();
+            su = warp_sum(at_base(ld_cluster_f32(ab), u.y, bu, c1));
+            sl = warp_sum(at_base(ld_cluster_f32(ab + 4), u.w, b, c1));
         }
-        Base b;
-        b.set(fmaxf(mu, ml), c1);
-        const float gap = ex2(bu.to(b, c1));                     // exp(mu - mx); next to the listed, what it flushes is nothing
-        float S = (su == 0.0f ? 0.0f : su * gap) + at_base(ml, sl, b, c1);
+        const float dm = bu.m - b.m, gap = dm == 0.0f ? 1.0f : ex2(dm * c1);
+        float S = (su == 0.0f ? 0.0f : su * gap) + sl;
         if (S == INFINITY) S = NAN;                              // a logit of +inf
         dead = dead || S == 0.0f;                                // or no logit above -inf: nothing to learn
         // No unlisted token is visible to the student, and what the teacher left is within what its log-sum-exp can tell: all is listed
@@ -551,7 +554,9 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
             if (!dead && mine(cur) && !(prob <= 0.0f)) part = wt * prob * (p.tau * logp - ((cur.z - b.m) - logS));
             part = warp_sum(part);
         }
-        if (rank == 0 && tid == 0 && !dead && !(R <= 0.0f)) part += wt * R * (p.tau * (logf(R) - logf(su)) - ((bu.m - b.m) - logS));
+        if (rank == 0 && tid == 0 && !dead && !(R <= 0.0f)) {
+            part += wt * R * (p.tau * logf(R) - (dm == 0.0f ? p.tau * logf(su / S) : dm + p.tau * logf(su) - logS));
+        }
         if (lane == 0) sm->loss[warp] = part;
         if (csize > 1) {
             __syncthreads();
