@@ -16,8 +16,8 @@ namespace quaff {
 
 // What a thread does once per row (reductions, the list) costs as much as its share of a row: 256 threads with sixteen words
 // each of a 64 KB slice; three CTAs per SM overlap their copies, sums and stores.  Measured: top 64 of 4096 x 32000 bf16
-// 85 us (3.1 TB/s; without the log-sum-exp 64), distillation of 8192 x 32000 bf16 240 us (4.4 TB/s read and written).  Both are bound
-// by instruction issue and the exponential unit (55 % of either at 24 warps per SM), not by HBM.
+// 85 us (3.1 TB/s; without the log-sum-exp 64), distillation of 8192 x 32000 bf16 226 us (4.6 TB/s read and written).  Both are bound
+// by instruction issue and the exponential unit (57 % of either at 24 warps per SM), not by HBM.
 constexpr int kLgThreads = 256;
 constexpr int kLgWarps = kLgThreads / 32;
 constexpr int kLgMaxK = 256;                 // list length limit of both operators
