@@ -293,10 +293,17 @@ __global__ void __launch_bounds__(kMxThreads, 1) mx4_gemm_kernel(const __grid_co
             bool ok = true;
             for (int tile = unit; tile < ntiles && ok; tile += nunits) {
                 for (int b = 0; b < p.nblk; ++b) {
+                    // Two things have to be over.  The MMAs that read this slot: their commit freed their stage, or, a full round of the ring
+                    // later, the stage of the position one round before this one.  And that position itself, which may be a stage of the adapters
+                    // that this warp passes over: until it is filled and used, the parity of its barrier is the one waited for below, and the
+                    // wait would end before the copies of this position have landed.  (Neither barrier can be two phases off: what this
+                    // warp saw filled last had waited for every position up to ten before this one, and nothing from here on is used without its scales.)
+                    if (n >= kMxSfSlots && pos - old_pos < kMxStages) {
+                        if (!mbar_wait(empty0 + 8u * old.stage, old.phase, abort_flag)) { ok = false; break; }
+                    } else if (pos >= kMxStages) {
+                        if (!mbar_wait(empty0 + 8u * ring.stage, ring.phase ^ 1u, abort_flag)) { ok = false; break; }
+                    }
                     if (n >= kMxSfSlots) {
-                        // The MMAs that read this slot are done: their commit freed their stage.  (A full round of the ring later
-                        // that stage has been filled again, which says the same, and its barrier is a phase further.)
-                        if (pos - old_pos < kMxStages && !mbar_wait(empty0 + 8u * old.stage, old.phase, abort_flag)) { ok = false; break; }
                         uint32_t step = 1;
                         if (++old_b == p.nblk) { old_b = 0; step += (uint32_t)p.lora_parts; }
                         old.next(step);

@@ -123,7 +123,7 @@ class Mx4Linear:
         forward : quaff_mx4_linear_fwd      backward: quaff_mx4_linear_bwd
 
     ``saved`` holds what the last forward leaves for its backward, (X, T); a caller that runs the backward of another batch
-    sets it.  With ``train=False`` no gradient buffers are made.  With it the workspace ``ws`` has room for the weight in bf16, 2 bytes per weight
+    sets it.  With ``train=False`` no gradient buffers are made.  Made for training, its workspace ``ws`` has room for the weight in bf16, 2 bytes per weight
     beside the 17/32 that it is held in; layers that run one after the other on one stream may share one (assign the largest to each).
 
     Y has rows of whole 16-byte words whatever N is, as quaff_distill_topk and ``backward`` take them (N columns of a wider buffer where
