@@ -8,7 +8,7 @@
 //   warps 2..5    : epilogue - tcgen05.ld, bf16 stores of dX, fp32 stores of the outlier partial products
 //   warps 6..21   : converters - raw INT8 tile -> bf16 B operand tile in the layout the MMA reads
 //
-// Two rings per CTA.  The IN ring (as many slots as fit, 7 on the benchmark shapes) receives what TMA brings: A = 128 rows
+// Two rings per CTA.  The IN ring (as many slots as fit: 6) receives what TMA brings: A = 128 rows
 // of dY x 64 contraction elements (16 KB) and RAW = 64 contraction rows x 128 INT8 codes (8 KB, 128-byte swizzle, as TMA
 // wrote it), plus the 64 step sizes dW[n] of those rows.  It is deep because it has to cover the latency of HBM.  The B
 // ring (4 slots of 16 KB) holds this CTA's half of the tile's output columns x 64 contraction rows as bf16 in the MN-major
@@ -362,8 +362,13 @@ __global__ void __launch_bounds__(kBxThreads, 1) bwd_expand_kernel(const __grid_
                 const uint32_t par = (raw_parity >> in_slot) & 1u;
                 raw_parity ^= 1u << in_slot;
                 if (ring.j == grp) {
-                    if (!mbar_wait(rawfull0 + 8u * in_slot, par, abort_flag)) { ok = false; break; }
+                    // In this order: the raw tile this slot held last went to another group, which may still be waiting for it, and until it has landed
+                    // the parity of its barrier is the one waited for here.  bfree says that the block four before this one and all before that are
+                    // over; with six slots (bx_stages) the slot's last raw tile is one of them, unless blocks and the stages of the adapters
+                    // alternate (one block per tile): then the slot itself has to have been given back.
                     if (!mbar_wait(bfree0 + 8u * grp, ring.jph ^ 1u, abort_flag)) { ok = false; break; }
+                    if (p.nblk == 1 && !mbar_wait(empty0 + 8u * in_slot, ring.iph ^ 1u, abort_flag)) { ok = false; break; }
+                    if (!mbar_wait(rawfull0 + 8u * in_slot, par, abort_flag)) { ok = false; break; }
                     // the step size of this thread's row: from the ring (no global load may be in flight when the proxy
                     // fence below is reached: it waits for every outstanding memory operation of the thread)
                     const int nrow = b * 64 + crow;

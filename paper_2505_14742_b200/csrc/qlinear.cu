@@ -267,7 +267,7 @@ static size_t bx_smem_bytes(int nstages, int mask_words) {     // ... plus the I
 }
 static int bx_stages(int mask_words) {
     const int fit = (int)((kSmemLimit - bx_fixed_bytes(mask_words)) / (kBxInBytes + 256));
-    return max(2, min(fit, kMaxStages));
+    return min(fit, kMaxStages);       // 6, up to the widest mask (K = 32768): the converters' waits rely on it
 }
 static quaff_status_t launch_bwd_expand(const BxParams& p, cudaStream_t st) {
     static std::atomic<bool> configured[64];
