@@ -170,9 +170,9 @@ __device__ __forceinline__ void as_they_arrive(int nb, F f) {
 
 // ------------------------------------------------------------------ exponentials relative to a maximum
 // 2^((z - max) c1).  The many terms are taken as 2^(z c1 - shift), shift = max c1 rounded: one fused multiply-add, two elements
-// per instruction; what the rounding of the shift adds to every exponent alike is taken out of their sum.  Where max c1
-// would overflow (masks of the type's lowest value fill the row) floats next to the maximum are so far apart that all but
-// the maximum itself vanish: a power of two that keeps the product exact and in range stands in for c1.
+// per instruction; what the rounding of the shift adds to every exponent alike is taken out of their sum.  That is up to 2^-25 of the shift, so
+// it has to stay small: from |max c1| = 2^31 on (finite masks fill the words) floats next to the maximum are 128 and more apart
+// in the exponent, and all but the maximum itself vanish; a power of two that keeps the product exact stands in for c1.
 typedef unsigned long long f32x2;
 __device__ __forceinline__ f32x2 pack2(float a, float b) {
     f32x2 r;
@@ -201,8 +201,8 @@ struct Base {              // a maximum as the exponentials take it
         m = fabsf(mx) == INFINITY ? 0.0f : mx;
         mul = c1;
         shift = m * c1;
-        if (!(fabsf(shift) < 1e38f)) {
-            mul = __uint_as_float(((127u + 60u + 127u) << 23) - (__float_as_uint(m) & 0x7F800000u));      // 2^60 / 2^exponent
+        if (!(fabsf(shift) < 0x1p31f)) {
+            mul = __uint_as_float(((127u + 31u + 127u) << 23) - (__float_as_uint(m) & 0x7F800000u));      // 2^31 / 2^exponent (that of m is -96 at least: c1 < 2^127)
             shift = m * mul;
         }
     }

@@ -30,6 +30,7 @@ def reference(Z, val, idx, lse, tau, w):
     M, V = z.shape
     loss, mag, grad, lim = np.zeros(M), np.zeros(M), np.zeros((M, V)), np.zeros((M, V))
     for m in range(M):
+        z[m] -= z[m].max()                                    # (beside a mask of 1e15 a double holds no logarithm)
         ok = (idx[m] >= 0) & (idx[m] < V) & (val[m] > -np.inf)
         at, t = idx[m][ok], val[m][ok].astype(np.float64) / tau
         logp = t - (lse64(t) if lse is None else float(lse[m]))
@@ -75,7 +76,9 @@ def check(Z, val, idx, lse, tau, w):
     if Z.dtype == torch.bfloat16:
         lim = lim + 2.0 ** -8 * np.abs(grad)
     assert np.isfinite(want).all() and np.isfinite(grad).all()
-    assert (np.abs(loss - want) <= 1e-5 * mag + 5e-6 * w * tau * tau).all(), (loss, want)
+    over = mag > 3.4e38                                        # beyond the floats
+    assert (loss[over] == INF).all()
+    assert (np.abs(loss - want) <= 1e-5 * mag + 5e-6 * w * tau * tau)[~over].all(), (loss, want)
     bad = ~(np.abs(dZ - grad) <= lim)
     assert not bad.any(), (np.argwhere(bad)[:4], dZ[bad][:4], grad[bad][:4])
 
