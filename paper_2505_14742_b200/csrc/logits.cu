@@ -479,10 +479,11 @@ __global__ void __launch_bounds__(kLgThreads, 3) distill_kernel(const DistillPar
                 const float tm = slots_max(l.x);
                 Base tb;
                 tb.set(tm, c1);
-                logP = logf(slots_sum(at_base(l.x, l.y, tb, c1)));
+                const float sum = slots_sum(at_base(l.x, l.y, tb, c1));
+                logP = logf(sum);
                 dead = tm == -INFINITY;                          // nothing listed
                 if (tm == INFINITY) c = logP = NAN;              // a listed value of +inf: inf / inf
-                if (listed) { logp = (cur.t - tb.m) * p.inv_tau - logP; prob = ex2(logp * kLog2e); }
+                if (listed) { logp = (cur.t - tb.m) * p.inv_tau - logP; prob = ex2((cur.t - tb.m) * c1) / sum; }      // (that of the largest has no error of ex2)
             }
         }
         if (csize > 1) {
