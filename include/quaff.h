@@ -373,7 +373,7 @@ quaff_status_t quaff_topk_logits(const void* Z, int z_dtype, int64_t ldz, int M,
  *   t_lse_opt null :  p_j = softmax over the list,              R = 0
  *   loss[m]  = w tau^2 ( sum_j p_j log(p_j / q_j) + R log(R / r) ),   r = the sum of q over the unlisted tokens
  *   dZ[m][v] = w tau (c q_v - p_v) for listed v,   w tau q_v (c - R / r) for the others,   c = sum p + R
- * (log r and q_v / r are taken relative to the largest unlisted logit: r itself may be less than any float)
+ * (where r is less than any float, log r and q_v / r are taken relative to the largest unlisted logit)
  * which is d loss[m] / d Z[m][v]: w = row_w_opt[m] is the gradient that arrives at the row's loss (1 / number of tokens, 0
  * for a token without a loss); null means 1.
  *   Z [M][V] bf16 or f32 (z_dtype), 16-byte aligned rows;  t_val [M][k] f32, t_idx [M][k] int32, dense;  1 <= k <= 256;  temperature as above
